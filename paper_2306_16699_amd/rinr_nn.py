@@ -8,6 +8,7 @@ memory come from the stream that works on them, and what the caller passes has t
 from __future__ import annotations
 
 import ctypes as C
+import math
 import struct
 from typing import Optional
 
@@ -56,17 +57,20 @@ def _require(ok: bool, what: str):
 
 class Packed8:
     """A matrix in 8 bits: codes int8 [rows, whole blocks of 32 columns], scales uint8 [rows, blocks], and how many columns there are;
-    the value is code * 2^(scale - 127).  `shape` is that of the tensor it stands for."""
-    __slots__ = ("_codes", "_scales", "_both", "rows", "cols", "ld", "shape", "device")
+    the value is code * 2^(scale - 127).  `shape` is that of the tensor it stands for: any leading dimensions of `rows` rows in all, and the
+    columns.  What a Packed8 says of itself cannot be set: results are allocated by it."""
+    __slots__ = ("_codes", "_scales", "_both", "_rows", "_cols", "_ld", "_shape", "_device")
 
     def __init__(self, codes, scales, cols: int, shape=None):
         _require(codes.dtype == torch.int8 and scales.dtype == torch.uint8 and codes.dim() == 2 and cols >= 1, "Packed8: int8 codes, uint8 scales")
         rows, blocks = codes.shape[0], (cols + BLOCK - 1) // BLOCK
         _require(codes.is_contiguous() and scales.is_contiguous() and codes.device == scales.device, "Packed8: contiguous, on one device")
         _require(tuple(codes.shape) == (rows, blocks * BLOCK) and tuple(scales.shape) == (rows, blocks), "Packed8: whole blocks of 32 columns")
+        shape = (rows, cols) if shape is None else tuple(shape)
+        _require(len(shape) >= 1 and shape[-1] == cols and all(n >= 0 for n in shape) and math.prod(shape[:-1]) == rows,
+                 f"Packed8: a shape of {rows} rows of {cols} columns")
         self._codes, self._scales, self._both = codes, scales, None
-        self.rows, self.cols, self.ld, self.device = rows, cols, blocks * BLOCK, codes.device
-        self.shape = (rows, cols) if shape is None else tuple(shape)
+        self._rows, self._cols, self._ld, self._device, self._shape = rows, cols, blocks * BLOCK, codes.device, shape
 
     @classmethod
     def _new(cls, on, like, rows: int, cols: int, shape):
@@ -75,30 +79,36 @@ class Packed8:
         blocks = (cols + BLOCK - 1) // BLOCK
         p._codes = p._scales = None
         p._both = on.empty(like, (rows * blocks * (BLOCK + 1),), torch.int8)
-        p.rows, p.cols, p.ld, p.shape, p.device = rows, cols, blocks * BLOCK, shape, on.dev
+        p._rows, p._cols, p._ld, p._shape, p._device = rows, cols, blocks * BLOCK, shape, on.dev
         return p
 
     def _pointers(self):
         if self._both is None:
             return self._codes.data_ptr(), self._scales.data_ptr()
         at = self._both.data_ptr()
-        return at, at + self.rows * self.ld
+        return at, at + self._rows * self._ld
+
+    rows = property(lambda self: self._rows)
+    cols = property(lambda self: self._cols)
+    ld = property(lambda self: self._ld)
+    shape = property(lambda self: self._shape)
+    device = property(lambda self: self._device)
 
     @property
     def codes(self):
         if self._codes is None:
-            self._codes = self._both[:self.rows * self.ld].view(self.rows, self.ld)
+            self._codes = self._both[:self._rows * self._ld].view(self._rows, self._ld)
         return self._codes
 
     @property
     def scales(self):
         if self._scales is None:
-            self._scales = self._both[self.rows * self.ld:].view(torch.uint8).view(self.rows, self.ld // BLOCK)
+            self._scales = self._both[self._rows * self._ld:].view(torch.uint8).view(self._rows, self._ld // BLOCK)
         return self._scales
 
     @property
     def nbytes(self) -> int:
-        return self.rows * (self.ld + self.ld // BLOCK)
+        return self._rows * (self._ld + self._ld // BLOCK)
 
 
 def _fail(what: str):
@@ -201,7 +211,7 @@ def _operand(x, dtype, dt: int, what: str):
         if x.device.type != "cuda":
             _fail(what + ": on the GPU")
         pc, ps = x._pointers()
-        return pc, x.rows, x.cols, x.ld, ps, PACKED8
+        return pc, x._rows, x._cols, x._ld, ps, PACKED8
     if x.dtype != dtype:
         _fail(f"{what}: {dtype} or Packed8")
     p, rows, cols, step = _mat(x, what)
@@ -264,7 +274,7 @@ def linear(x, w, bias=None, act: str = "none", w0: float = 30.0, residual=None, 
         z, pz, ldz, psz, tz = None, 0, 0, 0, 0
         if keep_z == "packed":
             z = Packed8._new(on, w, rows, n_out, shape)
-            (pz, psz), ldz, tz = z._pointers(), z.ld, PACKED8
+            (pz, psz), ldz, tz = z._pointers(), z._ld, PACKED8
         elif keep_z is not None:
             z = on.empty(w, shape, dtype)
             pz, ldz, tz = z.data_ptr(), n_out, dt
@@ -326,7 +336,7 @@ def rms_norm(x, gain, eps: float = 1e-6, residual=None, packed: bool = False, st
         h = x if residual is None else on.empty(x, shape, dtype)
         if packed:
             y = Packed8._new(on, x, rows, cols, tuple(shape))
-            (py, psy), ldy, ty = y._pointers(), y.ld, PACKED8
+            (py, psy), ldy, ty = y._pointers(), y._ld, PACKED8
         else:
             y = on.empty(x, shape, dtype)
             py, ldy, psy, ty = y.data_ptr(), cols, 0, dt

@@ -177,3 +177,20 @@ def test_no_workspace_for_no_rows():
     assert L.rinr_linear_workspace_bytes(linear_args(rows=0)) == 0
     assert L.rinr_linear_backward_workspace_bytes(grad_args(rows=0)) == 0
     assert L.rinr_rms_norm_backward_workspace_bytes(0, 8) == 0
+
+
+def test_a_packed_matrix_has_the_shape_of_its_rows():
+    """Results are allocated by a Packed8's shape and written by its rows: one says the other."""
+    codes, scales = torch.zeros(24, 64, dtype=torch.int8), torch.ones(24, 2, dtype=torch.uint8)
+    for shape in ((2, 48), (24, 64), (24, 47), (23, 48), (25, 48), (), (48,), (2, 3, 5, 48), (-4, -6, 48), (24, 48, 1), (0, 48)):
+        with pytest.raises(rinr.RinrError) as e:
+            rinr_nn.Packed8(codes, scales, 48, shape=shape)
+        assert e.value.code == rinr.E_ARG, shape
+    for shape in (None, (24, 48), (2, 3, 4, 48), torch.Size((24, 1, 48))):
+        p = rinr_nn.Packed8(codes, scales, 48, shape=shape)
+        assert p.shape == ((24, 48) if shape is None else tuple(shape)) and (p.rows, p.cols, p.ld) == (24, 48, 64)
+    assert rinr_nn.Packed8(codes[:1], scales[:1], 48, shape=(48,)).shape == (48,)
+    assert rinr_nn.Packed8(codes[:0], scales[:0], 48, shape=(3, 0, 48)).shape == (3, 0, 48)
+    for name in ("shape", "rows", "cols", "ld", "device", "codes", "scales"):
+        with pytest.raises(AttributeError):
+            setattr(p, name, getattr(p, name))

@@ -17,6 +17,9 @@
  * uint8[rows][ld / 32].  Such a value has 7 significant bits, so bf16 (and f16 within its range; beyond it values saturate at the
  * largest finite one) hold it exactly, and products take it as it stands.
  *
+ * At an infinity activations and slopes are their limits (GELU and SiLU: +inf and 1, 0 and 0); the sine's are NaN.  So a z kept in f16, infinite
+ * beyond 65504, has the gradient that the finite one has, but for the sine.
+ *
  * Sums (products, norms, gradients of bias and gain) are held in 32 bits.  Products of 32-bit operands take each operand as three
  * bf16 parts that add up to it and leave out what is below 2^-22 of a product; an infinity in such an operand makes results
  * NaN where 32-bit arithmetic would keep the infinity.  Results are the same bits from call to call on one GPU.

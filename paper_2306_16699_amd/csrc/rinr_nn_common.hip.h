@@ -178,6 +178,11 @@ __device__ __forceinline__ float turns(float z, const Act &a) {
     return __builtin_amdgcn_fractf(r) + __builtin_fmaf(z, a.turn_lo, __builtin_fmaf(z, a.turn_hi, -r));
 }
 
+// Beyond these the bell and exp(-|z|) are 0 in 32 bits.  z itself is held to them wherever it is multiplied by what has vanished there, so that an infinity
+// gives the limit and no NaN; a NaN stays one by the other factor.  (A z kept in f16 is infinite beyond 65504.)
+constexpr float kGeluFlat = 16.0f, kSiluFlat = 128.0f;
+__device__ __forceinline__ float held(float z, float low, float high) { return __builtin_amdgcn_fmed3f(z, low, high); }
+
 // Eight values through an activation; eight gradients times its slopes at z
 __device__ __forceinline__ void act_all(float (&v)[8], const Act &a) {
     switch (a.kind) {
@@ -187,11 +192,11 @@ __device__ __forceinline__ void act_all(float (&v)[8], const Act &a) {
             break;
         case RINR_ACT_GELU:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(-__builtin_fabsf(v[i]), gauss_of(v[i]).upper, __builtin_fmaxf(v[i], 0.0f));
+            for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(-__builtin_fabsf(held(v[i], -kGeluFlat, kGeluFlat)), gauss_of(v[i]).upper, __builtin_fmaxf(v[i], 0.0f));
             break;
         case RINR_ACT_SILU:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= sigmoid(v[i]);
+            for (int i = 0; i < 8; ++i) v[i] = held(v[i], -kSiluFlat, __builtin_inff()) * sigmoid(v[i]);
             break;
         case RINR_ACT_SINE:
 #pragma unroll
@@ -210,14 +215,14 @@ __device__ __forceinline__ void slope_all(float (&d)[8], const float (&z)[8], co
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const Gauss g = gauss_of(z[i]);
-                d[i] *= __builtin_fmaf(z[i] * 0.39894228040143268f, g.bell, 0.5f + __builtin_copysignf(0.5f - g.upper, z[i]));
+                d[i] *= __builtin_fmaf(held(z[i], -kGeluFlat, kGeluFlat) * 0.39894228040143268f, g.bell, 0.5f + __builtin_copysignf(0.5f - g.upper, z[i]));
             }
             break;
         case RINR_ACT_SILU:
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float g = sigmoid(z[i]);
-                d[i] *= g * (1.0f + z[i] * (1.0f - g));
+                d[i] *= g * (1.0f + held(z[i], -kSiluFlat, kSiluFlat) * (1.0f - g));
             }
             break;
         case RINR_ACT_SINE:

@@ -71,7 +71,8 @@ int rinr_linear(const rinr_linear_args *a, void *workspace, size_t workspace_byt
  * dz = dy act'(z), dx = dz w, dw = dz' x, dbias = sum of dz's rows.
  * With x_act, x holds what an activation was taken of (a z that the layer before kept): the layer's input was x_act(x), dw is taken
  * with that, and dx is the gradient of x before x_act: dx = (dz w) x_act'(x).
- * dx, dw, dbias: each may be NULL.  dz is rounded to dtype once, for both products; dbias is summed before that. */
+ * dx, dw, dbias: each may be NULL.  dz is rounded to dtype once, for both products; dbias is summed before that.  x_act(x) is rounded to dtype for dw, but
+ * where dz is rounded too (both activations, 16 bits): there it is taken as two of dtype, so that one rounding at most adds to the result's own. */
 typedef struct {
     int64_t rows, n_in, n_out;
     const void *dy; int64_t ld_dy;         /* dtype [rows][n_out]                                                    */

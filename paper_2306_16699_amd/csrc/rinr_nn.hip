@@ -230,9 +230,11 @@ int check_linear_grad(const rinr_linear_grad_args *a) {
 }
 
 // Where things lie in the workspace of a backward pass (dz, the layer's input where it is not kept as it is, and partial sums, which the
-// kernels use one after the other), and its two products.
+// kernels use one after the other), and its two products.  dz and x_act(x) are rounded to the operands' type, because matrix instructions of 16 bits take them so:
+// either one makes dw's error at most sqrt 2 of that of rounding dw alone.  Both together would make it sqrt 3, so x_act(x) is then taken in two parts: the product
+// runs over twice the rows, dz twice and the parts one below the other (2000 x 500 -> 300: 1.65 of a rounding, and 1.41 in two parts).
 struct GradPlan {
-    int64_t ld_dz, ld_xa, sum_chunks, rows_each;
+    int64_t ld_dz, ld_xa, sum_chunks, rows_each, dw_rows;
     size_t xa, part, bytes;
     Side dx_p, dx_q, dw_p, dw_q;
     Plan dx, dw;
@@ -243,15 +245,16 @@ GradPlan grad_plan(const rinr_linear_grad_args *a, char *ws) {
     size_t part = 0;
     Side dz = {a->dy, a->ld_dy, 0, nullptr}, x = {a->x, a->ld_x, a->n_in, a->x_scales};
     const bool packed = a->x_type == RINR_T_PACKED8;
+    g.dw_rows = a->rows * (a->dw && a->act != RINR_ACT_NONE && a->x_act != RINR_ACT_NONE && a->dtype != RINR_T_F32 ? 2 : 1);
     if (a->act != RINR_ACT_NONE && (a->dx || a->dw)) {
         g.ld_dz = round_up(a->n_out, 64);
-        g.xa = (size_t)round_up((int64_t)((size_t)a->rows * (size_t)g.ld_dz * el), 256);
+        g.xa = (size_t)round_up((int64_t)((size_t)g.dw_rows * (size_t)g.ld_dz * el), 256);
         dz = {ws, g.ld_dz, 0, nullptr};
     }
     g.part = g.xa;
     if (a->dw && (packed || a->x_act != RINR_ACT_NONE)) {
         g.ld_xa = round_up(a->n_in, 64);
-        g.part += (size_t)round_up((int64_t)((size_t)a->rows * (size_t)g.ld_xa * el), 256);
+        g.part += (size_t)round_up((int64_t)((size_t)g.dw_rows * (size_t)g.ld_xa * el), 256);
         x = {ws + g.xa, g.ld_xa, a->n_in, nullptr};
     }
     const int64_t across = div_up(g.ld_dz ? g.ld_dz : a->n_out, 256);
@@ -270,7 +273,7 @@ GradPlan grad_plan(const rinr_linear_grad_args *a, char *ws) {
         g.dw_p = x;
         g.dw_q = dz;
         g.dw_q.n = a->n_out;
-        g.dw = plan_of(a->dtype, kGradW, false, false, g.dw_p, g.dw_q, a->rows);
+        g.dw = plan_of(a->dtype, kGradW, false, false, g.dw_p, g.dw_q, g.dw_rows);
         part = std::max(part, part_bytes(g.dw, a->n_in, a->n_out));
     }
     g.bytes = g.part + (size_t)round_up((int64_t)part, 256);
@@ -283,17 +286,27 @@ template <class T> void launch_slope(const SlopeArgs &s, int64_t across, int64_t
 void launch_sum_parts(const float *part, int64_t n, int64_t cols, float *out, hipStream_t st) {
     hipLaunchKernelGGL(sum_parts_kernel, dim3((uint32_t)div_up(cols, 32)), dim3(1024), 0, st, part, n, cols, out);
 }
-template <class T> void launch_unpack(int64_t rows, int64_t cols, const void *codes, int64_t ld, const uint8_t *scales, const Act &act, void *x, int64_t ld_x, hipStream_t st) {
-    hipLaunchKernelGGL(unpack_kernel<T>, dim3((uint32_t)div_up(rows * div_up(cols, 8), 256)), dim3(256), 0, st, rows, (int)cols, (const int8_t *)codes, ld, scales, act, (T *)x, ld_x,
-                       rows * cols * (int64_t)sizeof(T) > kPastL2);
+template <class T, bool LOW> void launch_unpack(int64_t rows, int64_t cols, const void *codes, int64_t ld, const uint8_t *scales, const Act &act, void *x, int64_t ld_x, hipStream_t st) {
+    hipLaunchKernelGGL((unpack_kernel<T, LOW>), dim3((uint32_t)div_up(rows * div_up(cols, 8), 256)), dim3(256), 0, st, rows, (int)cols, (const int8_t *)codes, ld, scales, act, (T *)x,
+                       ld_x, rows * cols * (int64_t)sizeof(T) > kPastL2);
+}
+template <class T> void launch_values(int64_t rows, int64_t cols, const void *codes, int64_t ld, const uint8_t *scales, const Act &act, void *x, int64_t ld_x, hipStream_t st) {
+    launch_unpack<T, false>(rows, cols, codes, ld, scales, act, x, ld_x, st);
 }
 template <class T> void launch_pack(uint32_t blocks, int64_t rows, int64_t cols, const void *x, int64_t ld_x, void *codes, int64_t ld, uint8_t *scales, hipStream_t st) {
     hipLaunchKernelGGL(pack_kernel<T>, dim3(blocks), dim3(256), 0, st, rows, (int)cols, (const T *)x, ld_x, (int8_t *)codes, ld, scales, rows * cols > kPastL2);
 }
-template <class T> void launch_act(int64_t rows, int64_t cols, const void *z, int64_t ld, const uint8_t *scales, bool packed, const Act &act, void *x, int64_t ld_x, hipStream_t st) {
-    if (packed) launch_unpack<T>(rows, cols, z, ld, scales, act, x, ld_x, st);
-    else hipLaunchKernelGGL(act_kernel<T>, dim3((uint32_t)div_up(rows * div_up(cols, 8), 256)), dim3(256), 0, st, rows, (int)cols, (const T *)z, ld, act, (T *)x, ld_x,
+template <class T, bool LOW> void launch_act_parts(int64_t rows, int64_t cols, const void *z, int64_t ld, const uint8_t *scales, bool packed, const Act &act, void *x, int64_t ld_x,
+                                                   hipStream_t st) {
+    if (packed) launch_unpack<T, LOW>(rows, cols, z, ld, scales, act, x, ld_x, st);
+    else hipLaunchKernelGGL((act_kernel<T, LOW>), dim3((uint32_t)div_up(rows * div_up(cols, 8), 256)), dim3(256), 0, st, rows, (int)cols, (const T *)z, ld, act, (T *)x, ld_x,
                             rows * cols * (int64_t)sizeof(T) > kPastL2);
+}
+// two_parts: of 16-bit types only
+template <class T> void launch_act(int64_t rows, int64_t cols, const void *z, int64_t ld, const uint8_t *scales, bool packed, const Act &act, void *x, int64_t ld_x, bool two_parts,
+                                   hipStream_t st) {
+    if (sizeof(T) == 2 && two_parts) launch_act_parts<T, sizeof(T) == 2>(rows, cols, z, ld, scales, packed, act, x, ld_x, st);
+    else launch_act_parts<T, false>(rows, cols, z, ld, scales, packed, act, x, ld_x, st);
 }
 
 // ---- norms ---------------------------------------------------------------------------------------------------------------------------
@@ -362,7 +375,7 @@ extern "C" int rinr_linear(const rinr_linear_args *a, void *workspace, size_t wo
     if (workspace_bytes < l.bytes) return RINR_E_SIZE;
     if (l.bytes && !aligned(workspace, 16)) return RINR_E_ALIGN;
     float *const part = (float *)((char *)workspace + l.x);
-    if (l.ld_x) NN_BY_TYPE(a->dtype, launch_act, a->rows, a->n_in, a->x, a->ld_x, a->x_scales, true, make_act(RINR_ACT_NONE, 0.0f), workspace, l.ld_x, (hipStream_t)stream);
+    if (l.ld_x) NN_BY_TYPE(a->dtype, launch_act, a->rows, a->n_in, a->x, a->ld_x, a->x_scales, true, make_act(RINR_ACT_NONE, 0.0f), workspace, l.ld_x, false, (hipStream_t)stream);
     Epilogue e = {};
     e.bias = a->bias;
     e.residual = a->residual;
@@ -404,7 +417,7 @@ extern "C" int rinr_linear_backward(const rinr_linear_grad_args *a, void *worksp
     if (g.ld_dz || a->dbias) {
         const SlopeArgs s = {a->rows, a->n_out, g.rows_each, a->dy, a->z, a->z_scales, g.ld_dz ? ws : nullptr, a->dbias ? part : nullptr,
                              a->ld_dy, a->ld_z, g.ld_dz, g.ld_dz ? g.ld_dz : a->n_out, a->z_type == RINR_T_PACKED8,
-                             past_l2(a->rows, a->n_out, a->dtype), make_act(a->act, a->w0)};
+                             past_l2(a->rows, a->n_out, a->dtype), g.dw_rows > a->rows, make_act(a->act, a->w0)};
         NN_BY_TYPE(a->dtype, launch_slope, s, div_up(s.cols_dz, 256), g.sum_chunks, st);
         if (a->dbias) launch_sum_parts(part, g.sum_chunks, a->n_out, a->dbias, st);
     }
@@ -423,12 +436,13 @@ extern "C" int rinr_linear_backward(const rinr_linear_grad_args *a, void *worksp
         NN_CHECK(product(a->dtype, kGradX, false, g.dx, g.dx_p, g.dx_q, a->n_out, e, part, st));
     }
     if (a->dw) {
-        if (g.ld_xa) NN_BY_TYPE(a->dtype, launch_act, a->rows, a->n_in, a->x, a->ld_x, a->x_scales, x_packed, make_act(a->x_act, a->w0), ws + g.xa, g.ld_xa, st);
+        if (g.ld_xa) NN_BY_TYPE(a->dtype, launch_act, a->rows, a->n_in, a->x, a->ld_x, a->x_scales, x_packed, make_act(a->x_act, a->w0), ws + g.xa, g.ld_xa, g.dw_rows > a->rows,
+                               st);
         Epilogue e = {};
         e.y = a->dw;
         e.ld_y = a->ld_dw;
         e.past = past_l2(a->n_out, a->n_in, a->dtype);
-        NN_CHECK(product(a->dtype, kGradW, false, g.dw, g.dw_p, g.dw_q, a->rows, e, part, st));
+        NN_CHECK(product(a->dtype, kGradW, false, g.dw, g.dw_p, g.dw_q, g.dw_rows, e, part, st));
     }
     return launched();
 }
@@ -512,6 +526,6 @@ extern "C" int rinr_unpack8(int64_t rows, int64_t cols, const void *codes, int64
     NN_CHECK(check_mat(codes, ld, scales, RINR_T_PACKED8, cols));
     NN_CHECK(check_mat(x, ld_x, nullptr, dtype, cols));
     if (div_up(rows * div_up(cols, 8), 256) > INT32_MAX) return RINR_E_UNSUPPORTED;
-    NN_BY_TYPE(dtype, launch_unpack, rows, cols, codes, ld, scales, make_act(act, w0), x, ld_x, (hipStream_t)stream);
+    NN_BY_TYPE(dtype, launch_values, rows, cols, codes, ld, scales, make_act(act, w0), x, ld_x, (hipStream_t)stream);
     return launched();
 }

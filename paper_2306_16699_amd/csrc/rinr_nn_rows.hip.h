@@ -201,7 +201,21 @@ template <class T> __global__ __launch_bounds__(256) void pack_kernel(int64_t ro
     if (row < rows) store_packed(codes, scales, row, ld, col, cols, v, past);          // a block's four lanes have the same row
 }
 
-template <class T> __global__ __launch_bounds__(256) void unpack_kernel(int64_t rows, int cols, const int8_t *codes, int64_t ld, const uint8_t *scales, const Act act, T *x,
+// An activation's values as T; with LOW what T leaves of them, as T, `rows` rows further down (a product of both blocks takes them to twice T's bits)
+template <class T, bool LOW> __device__ __forceinline__ void store_act(T *x, int64_t row, int64_t rows, int64_t ld_x, int col, int64_t have, const float (&v)[8], bool past) {
+    store_n<T, 8>(x + row * ld_x + col, have, v, past);
+    if (LOW) {
+        float low[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float left = v[i] - (float)from_float<T>(v[i]);
+            low[i] = __builtin_fabsf(left) < __builtin_inff() ? left : 0.0f;     // of an infinity or a NaN nothing is left
+        }
+        store_n<T, 8>(x + (rows + row) * ld_x + col, have, low, past);
+    }
+}
+
+template <class T, bool LOW> __global__ __launch_bounds__(256) void unpack_kernel(int64_t rows, int cols, const int8_t *codes, int64_t ld, const uint8_t *scales, const Act act, T *x,
                                                                        int64_t ld_x, bool past) {
     const int64_t per_row = (cols + 7) / 8;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -213,10 +227,10 @@ template <class T> __global__ __launch_bounds__(256) void unpack_kernel(int64_t 
     kept.load(codes, scales, ld, true, row, col, cols - col);
     kept.get(true, v);
     act_all(v, act);
-    store_n<T, 8>(x + row * ld_x + col, cols - col, v, past);
+    store_act<T, LOW>(x, row, rows, ld_x, col, cols - col, v, past);
 }
 
-template <class T> __global__ __launch_bounds__(256) void act_kernel(int64_t rows, int cols, const T *z, int64_t ld_z, const Act act, T *x, int64_t ld_x, bool past) {
+template <class T, bool LOW> __global__ __launch_bounds__(256) void act_kernel(int64_t rows, int cols, const T *z, int64_t ld_z, const Act act, T *x, int64_t ld_x, bool past) {
     const int64_t per_row = (cols + 7) / 8;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t row = at / per_row;
@@ -225,7 +239,7 @@ template <class T> __global__ __launch_bounds__(256) void act_kernel(int64_t row
     float v[8];
     load_n<T, 8>(z + row * ld_z + col, cols - col, v);
     act_all(v, act);
-    store_n<T, 8>(x + row * ld_x + col, cols - col, v, past);
+    store_act<T, LOW>(x, row, rows, ld_x, col, cols - col, v, past);
 }
 
 // Zeros: `bytes` (a multiple of 2) at blockIdx.x * stride
@@ -243,7 +257,7 @@ struct SlopeArgs {
     void *dz;                                                                    // NULL: sums only
     float *part;                                                                 // [gridDim.y][cols], or NULL
     int64_t ld_dy, ld_z, ld_dz, cols_dz;                                         // dz has zeros from `cols` to cols_dz
-    bool packed, past;
+    bool packed, past, twice;                                                    // twice: dz once more, `rows` rows further down
     Act act;
 };
 
@@ -272,6 +286,7 @@ template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Slo
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += d[i];
             if (a.dz) store_n<T, 8>((T *)a.dz + row * a.ld_dz + col, a.cols_dz - col, d, a.past);
+            if (a.twice) store_n<T, 8>((T *)a.dz + (a.rows + row) * a.ld_dz + col, a.cols_dz - col, d, a.past);
         }
     }
     if (!a.part) return;

@@ -96,3 +96,36 @@ def test_what_f16_cannot_keep_has_its_gradient(act):
     same_z = z.clamp(-60000, 60000)
     for got, want in zip((dx, dw, db), nn.linear_backward(dy, x, w, act=act, z=same_z)):
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("act,x_act,packed", [("gelu", "gelu", False), ("silu", "gelu", True), ("gelu", "silu", True), ("sine", "sine", False), ("gelu", "none", False), ("none", "silu", True)])
+@pytest.mark.parametrize("rows,n_in,n_out", [(2000, 500, 300), (300, 257, 129), (40, 704, 700)])
+def test_gradients_carry_one_rounding_beside_their_own(rows, n_in, n_out, act, x_act, packed, dtype):
+    """dz is rounded to 16 bits on its way into the products, or x_act(x) is: with the result's own rounding, of like size and independent, the error's norm is
+    sqrt 2 of what rounding the exact result alone leaves (1.5: the spread of norms of some 10^4 values is a few percent), also where both are recomputed."""
+    dt = DTYPES[dtype]
+    g = gen(rows + n_in)
+    scale = 0.1 if act == "sine" else 1.0
+    w, dy = (torch.randn(*s, generator=g, device="cuda").to(dt) for s in ((n_out, n_in), (rows, n_out)))
+    x, z = (scale * torch.randn(*s, generator=g, device="cuda").to(dt) for s in ((rows, n_in), (rows, n_out)))
+    x = nn.pack8(x) if packed else x
+
+    def both(v, kind):
+        v = nn.unpack8(v, torch.float32).double() if isinstance(v, nn.Packed8) else v.double()
+        if kind == "none":
+            return v, torch.ones_like(v)
+        if kind == "gelu":
+            p = 0.5 * torch.special.erfc(-v / math.sqrt(2))
+            return v * p, p + v * torch.exp(-v * v / 2) / math.sqrt(2 * math.pi)
+        if kind == "silu":
+            s = torch.sigmoid(v)
+            return v * s, s * (1 + v * (1 - s))
+        return torch.sin(30.0 * v), 30.0 * torch.cos(30.0 * v)
+
+    dx, dw, _ = nn.linear_backward(dy, x, w, act=act, z=z if act != "none" else None, x_act=x_act)
+    dz = dy.double() * (both(z, act)[1] if act != "none" else 1.0)
+    xa, xs = both(x, x_act)
+    for got, want, what in ((dx, (dz @ w.double()) * xs, "dx"), (dw, dz.t().contiguous() @ xa, "dw")):
+        least = float((want.to(dt).double() - want).norm())
+        assert float((got.double() - want).norm()) <= 1.5 * least, (what, float((got.double() - want).norm()) / least)

@@ -75,7 +75,7 @@ template <class T> __device__ __forceinline__ void finish(const Epilogue &e, con
     }
     if (!there || have <= 0) return;
     if (e.z && !e.z_packed) store_n<T, 8>((T *)e.z + q * e.ld_z + p, have, v, e.past);
-    act_all(v, e.act);
+    act_all<T>(v, e.act);
     if (e.residual) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += (float)in.r[i];
@@ -83,7 +83,7 @@ template <class T> __device__ __forceinline__ void finish(const Epilogue &e, con
     if (e.slope) {
         float z[8];
         in.z.get(e.slope_packed, z);
-        slope_all(v, z, e.slope_act);
+        slope_all<T>(v, z, e.slope_act);
     }
     store_n<T, 8>((T *)e.y + q * e.ld_y + p, have, v, e.past);
 }

@@ -226,7 +226,7 @@ template <class T, bool LOW> __global__ __launch_bounds__(256) void unpack_kerne
     float v[8];
     kept.load(codes, scales, ld, true, row, col, cols - col);
     kept.get(true, v);
-    act_all(v, act);
+    act_all<T>(v, act);
     store_act<T, LOW>(x, row, rows, ld_x, col, cols - col, v, past);
 }
 
@@ -238,7 +238,7 @@ template <class T, bool LOW> __global__ __launch_bounds__(256) void act_kernel(i
     const int col = (int)(at - row * per_row) * 8;
     float v[8];
     load_n<T, 8>(z + row * ld_z + col, cols - col, v);
-    act_all(v, act);
+    act_all<T>(v, act);
     store_act<T, LOW>(x, row, rows, ld_x, col, cols - col, v, past);
 }
 
@@ -278,7 +278,7 @@ template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Slo
                     float z[8];
                     kept.load(a.z, a.z_scales, a.ld_z, a.packed, row, col, have);
                     kept.get(a.packed, z);
-                    slope_all(d, z, a.act);
+                    slope_all<T>(d, z, a.act);
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] = i < have ? d[i] : 0.0f;

@@ -129,3 +129,40 @@ def test_gradients_carry_one_rounding_beside_their_own(rows, n_in, n_out, act, x
     for got, want, what in ((dx, (dz @ w.double()) * xs, "dx"), (dw, dz.t().contiguous() @ xa, "dw")):
         least = float((want.to(dt).double() - want).norm())
         assert float((got.double() - want).norm()) <= 1.5 * least, (what, float((got.double() - want).norm()) / least)
+
+
+def gelu_and_slope(z, dtype):
+    """The kernels' GELU and its slope at a vector z of `dtype`: z as the whole of a layer's sum, and as what one row kept (its bias' gradient is in 32 bits)."""
+    n = z.numel()
+    y = nn.linear(torch.zeros(1, 8, device="cuda", dtype=dtype), torch.zeros(n, 8, device="cuda", dtype=dtype), z.float(), act="gelu")[0]
+    one = torch.ones(1, n, device="cuda", dtype=dtype)
+    s = nn.linear_backward(one, torch.zeros(1, 8, device="cuda", dtype=dtype), torch.zeros(n, 8, device="cuda", dtype=dtype), act="gelu", z=z[None], need_dx=False, need_dw=False)[2]
+    v = z.double()
+    p, d = 0.5 * torch.special.erfc(-v / math.sqrt(2)), torch.exp(-v * v / 2) / math.sqrt(2 * math.pi)
+    return y, s, v * p, p, v * d
+
+
+def test_gelu_in_32_bits_is_as_good_as_elementary_operations():
+    """Errors' norms for normal z, against those of z (1 + erf(z / sqrt 2)) / 2 and its derivative in elementary 32-bit operations: both have some four
+    roundings of like size, so neither is 1.5 of the other."""
+    z = torch.randn(400000, generator=gen(1), device="cuda")
+    y, s, y64, p64, zd64 = gelu_and_slope(z, torch.float32)
+    e = torch.erf(z * math.sqrt(0.5))
+    for got, plain, want in ((y, 0.5 * z * (1 + e), y64), (s, 0.5 * (1 + e) + z * torch.exp(-0.5 * z * z) * (1 / math.sqrt(2 * math.pi)), p64 + zd64)):
+        off, least = float((got.double() - want).norm()), float((plain.double() - want).norm())
+        assert off <= 1.5 * least, off / least
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gelu_keeps_its_tail(dtype):
+    """Far below 0 GELU and its slope are small, and right to their own size: the tail's polynomial to 5e-5 (32 bits: 1e-6), the bell's exponent z^2 / 2 to two
+    roundings, and a result's own rounding."""
+    dt = DTYPES[dtype]
+    z = torch.cat([-torch.linspace(0, 12.5, 20001, device="cuda"), torch.linspace(0, 12.5, 5001, device="cuda")]).to(dt)
+    y, s, y64, p64, zd64 = gelu_and_slope(z, dt)
+    v = z.double()
+    poly, bell = 1e-6 if dtype == "f32" else 5e-5, (3 + v * v) * 2.0 ** -23
+    tail = torch.minimum(p64, 1 - p64)
+    assert bool(((y.double() - y64).abs() <= (torch.finfo(dt).eps * 0.505 + 2.0 ** -23) * y64.abs() + v.abs() * tail * (poly + bell)
+                 + (2.0 ** -25 if dtype == "f16" else 2.0 ** -126)).all())
+    assert bool(((s.double() - p64 - zd64).abs() <= tail * (poly + bell) + zd64.abs() * bell + 2.0 ** -23 * (p64 + zd64.abs()) + 2.0 ** -126).all())

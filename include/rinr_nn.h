@@ -14,8 +14,9 @@
  * every 32 columns of a row (a block; the last may be shorter) share one scale byte e, the value is code * 2^(e - 127), codes are
  * -127..127, and e (1..254) is the least with which the block's largest value fits.  A block that holds an infinity or a NaN has
  * e = 255 and stands for NaN.  Codes: int8[rows][ld], ld a multiple of 32, 16-byte aligned, 0 behind the last column; scales:
- * uint8[rows][ld / 32].  Such a value has 7 significant bits, so bf16 (and f16 within its range; beyond it values saturate at the
- * largest finite one) hold it exactly, and products take it as it stands.
+ * uint8[rows][ld / 32].  Such a value has 7 significant bits, so bf16 (and f16 within its range) hold it exactly, and
+ * products take it as it stands.  Beyond the range of bf16 (in f16: of f16) it stands for the largest finite number there, so that a finite block never gives an
+ * infinity.
  *
  * At an infinity activations and slopes are their limits (GELU and SiLU: +inf and 1, 0 and 0); the sine's are NaN.  So a z kept in f16, infinite
  * beyond 65504, has the gradient that the finite one has, but for the sine.

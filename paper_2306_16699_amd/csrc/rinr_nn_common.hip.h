@@ -145,9 +145,16 @@ __device__ __forceinline__ void store_packed(int8_t *codes, uint8_t *scales, int
     }
 }
 
-// An element of type T from a packed value: beyond f16's range its largest finite number (the block was finite)
-template <class T> __device__ __forceinline__ float in_range(float v) { return v; }
-template <> __device__ __forceinline__ float in_range<f16>(float v) { return v > 65504.0f ? 65504.0f : (v < -65504.0f ? -65504.0f : v); }
+// What a packed value beyond T's range stands for: T's largest finite number; in 32 bits bf16's, so that a product and an unpacked value are the same.  (A
+// block whose largest is above 127.5 2^121 has codes of 64 and a scale of 2^122.)  Only scales from `first` on reach so far; 255 stays a NaN.
+template <class T> struct Reach { static constexpr float most = 0x1.fep127f; static constexpr uint32_t first = 249; };
+template <> struct Reach<f16> { static constexpr float most = 65504.0f; static constexpr uint32_t first = 137; };
+template <class T, int N> __device__ __forceinline__ void in_range(uint32_t byte, float (&v)[N]) {
+    if (byte - Reach<T>::first < 255u - Reach<T>::first) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_fmed3f(v[i], -Reach<T>::most, Reach<T>::most);
+    }
+}
 
 // ---- activations -------------------------------------------------------------------------------------------------------------------
 
@@ -275,8 +282,7 @@ template <class T> struct Kept {
             const float s = scale_of(byte);
             values_of(w[0], s, o);
             values_of(w[1], s, o + 4);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = in_range<T>(o[i]);
+            in_range<T>(byte, o);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = (float)v[i];

@@ -196,8 +196,9 @@ template <class E> struct Group<E, kPacked> {
         float f[8];
         values_of(there ? w[0] : 0u, sc, f);
         values_of(there ? w[1] : 0u, sc, f + 4);
+        in_range<E>(there ? byte : 0u, f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[0][i] = (E)in_range<E>(f[i]);
+        for (int i = 0; i < 8; ++i) o[0][i] = (E)f[i];
 #pragma unroll
         for (int n = 1; n < PARTS; ++n) o[n] = vec8<E>{};                        // 7 bits: the first part is all of it
     }
@@ -717,7 +718,10 @@ template <class T> struct TinySide {
     __device__ __forceinline__ float at(int64_t n, int64_t k) const {
         const int64_t row = k_rows ? k : n, col = k_rows ? n : k;
         if (!packed) return (float)((const T *)s.p)[row * s.ld + col];
-        return in_range<T>((float)((const int8_t *)s.p)[row * s.ld + col] * scale_of(s.scales[row * (s.ld / kBlock8) + col / kBlock8]));
+        const uint32_t byte = s.scales[row * (s.ld / kBlock8) + col / kBlock8];
+        float v[1] = {(float)((const int8_t *)s.p)[row * s.ld + col] * scale_of(byte)};
+        in_range<T>(byte, v);
+        return v[0];
     }
 };
 template <class T> __global__ __launch_bounds__(256) void tiny_kernel(const GemmArgs a, int64_t tasks, bool kp, bool kq, bool p_packed, bool q_packed) {

@@ -166,3 +166,39 @@ def test_gelu_keeps_its_tail(dtype):
     assert bool(((y.double() - y64).abs() <= (torch.finfo(dt).eps * 0.505 + 2.0 ** -23) * y64.abs() + v.abs() * tail * (poly + bell)
                  + (2.0 ** -25 if dtype == "f16" else 2.0 ** -126)).all())
     assert bool(((s.double() - p64 - zd64).abs() <= tail * (poly + bell) + zd64.abs() * bell + 2.0 ** -23 * (p64 + zd64.abs()) + 2.0 ** -126).all())
+
+
+MOST = {torch.bfloat16: torch.finfo(torch.bfloat16).max, torch.float16: 65504.0, torch.float32: torch.finfo(torch.bfloat16).max}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_a_finite_block_never_gives_an_infinity(dtype):
+    """The largest numbers, whose code and scale multiply to 2^128, and codes that a caller put together."""
+    dt = DTYPES[dtype]
+    most = MOST[dt]
+    for value in (torch.finfo(torch.float32).max, torch.finfo(torch.bfloat16).max, 1.9921875 * 2.0 ** 127):
+        x = torch.zeros(3, 64, device="cuda")
+        x[0, 5], x[1, 40], x[2, 0] = value, -value, 1.0
+        p = nn.pack8(x)
+        assert p.scales[0, 0] == 249 and p.codes[0, 5] == 64
+        want = torch.zeros(3, 64, device="cuda", dtype=torch.float64)
+        want[0, 5], want[1, 40], want[2, 0] = most, -most, 1.0
+        assert same(nn.unpack8(p, dt), want)
+        for rows in (1, 20, 33):                                       # a packed operand of few rows, and of more than 64
+            q = nn.Packed8(p.codes.repeat(rows, 1), p.scales.repeat(rows, 1), 64)
+            eye = torch.eye(64, device="cuda", dtype=dt)
+            assert same(nn.linear(q, eye), want.repeat(rows, 1)), rows
+        narrow = nn.Packed8(p.codes[:, :32].contiguous(), p.scales[:, :1].contiguous(), 6)
+        assert same(nn.linear(narrow, torch.eye(6, device="cuda", dtype=dt)[5:6].contiguous()), [[most], [0.0], [0.0]])
+        dw = nn.linear_backward(torch.ones(1, 40, device="cuda", dtype=dt), nn.Packed8(p.codes[:1], p.scales[:1], 64), torch.zeros(40, 64, device="cuda", dtype=dt))[1]
+        assert same(dw, want[:1].expand(40, 64))
+    b = torch.full((40,), torch.finfo(torch.float32).max, device="cuda")
+    for rows in (2, 100):                                              # kept by the layer, and the norm's
+        _, z = nn.linear(torch.zeros(rows, 16, device="cuda", dtype=dt), torch.zeros(40, 16, device="cuda", dtype=dt), b, keep_z="packed")
+        assert same(nn.unpack8(z, dt), most)
+        y, _ = nn.rms_norm(torch.ones(rows, 40, device="cuda", dtype=dt), b, packed=True)
+        assert same(nn.unpack8(y, dt), most)
+    codes, scales = torch.full((4, 32), 127, device="cuda", dtype=torch.int8), torch.tensor([[254], [249], [255], [1]], device="cuda", dtype=torch.uint8)
+    codes[0, 1], codes[1, 1], codes[2] = -127, 1, 0
+    got = nn.unpack8(nn.Packed8(codes, scales, 32), dt).double()
+    assert got[0, 0] == most and got[0, 1] == -most and got[1, 0] == most and got[1, 1] == min(2.0 ** 122, most) and torch.isnan(got[2]).all() and bool((got[3] < 1).all())

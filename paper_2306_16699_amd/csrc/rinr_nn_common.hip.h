@@ -95,7 +95,7 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t largest_bits) {
     const int e = (int)((largest_bits + 0x10000u) >> 23) - 6;
     return largest_bits >= 0x7f800000u ? 255u : (uint32_t)(e < 1 ? 1 : e);
 }
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }              // 255: infinity, and 0 times that a NaN
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }              // 255: in_range sees to it
 __device__ __forceinline__ float inverse_of(uint32_t byte) { return byte == 255u ? 0.0f : __uint_as_float((254u - byte) << 23); }
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 // Four codes of a block: v * inverse is exact, and adding 1.5 2^23 rounds it to a whole number in the sum's low bits.  A block of 255: 0.
@@ -146,13 +146,13 @@ __device__ __forceinline__ void store_packed(int8_t *codes, uint8_t *scales, int
 }
 
 // What a packed value beyond T's range stands for: T's largest finite number; in 32 bits bf16's, so that a product and an unpacked value are the same.  (A
-// block whose largest is above 127.5 2^121 has codes of 64 and a scale of 2^122.)  Only scales from `first` on reach so far; 255 stays a NaN.
+// block whose largest is above 127.5 2^121 has codes of 64 and a scale of 2^122.)  Only scales from `first` on reach so far.  A block of 255 is NaN, whatever its codes.
 template <class T> struct Reach { static constexpr float most = 0x1.fep127f; static constexpr uint32_t first = 249; };
 template <> struct Reach<f16> { static constexpr float most = 65504.0f; static constexpr uint32_t first = 137; };
 template <class T, int N> __device__ __forceinline__ void in_range(uint32_t byte, float (&v)[N]) {
-    if (byte - Reach<T>::first < 255u - Reach<T>::first) {
+    if (byte >= Reach<T>::first) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_fmed3f(v[i], -Reach<T>::most, Reach<T>::most);
+        for (int i = 0; i < N; ++i) v[i] = byte == 255u ? __builtin_nanf("") : __builtin_amdgcn_fmed3f(v[i], -Reach<T>::most, Reach<T>::most);
     }
 }
 

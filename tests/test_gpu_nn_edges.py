@@ -202,3 +202,21 @@ def test_a_finite_block_never_gives_an_infinity(dtype):
     codes[0, 1], codes[1, 1], codes[2] = -127, 1, 0
     got = nn.unpack8(nn.Packed8(codes, scales, 32), dt).double()
     assert got[0, 0] == most and got[0, 1] == -most and got[1, 0] == most and got[1, 1] == min(2.0 ** 122, most) and torch.isnan(got[2]).all() and bool((got[3] < 1).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_a_block_that_stands_for_nan_is_nan_whatever_its_codes(rows, dtype):
+    dt = DTYPES[dtype]
+    codes, scales = torch.full((rows, 64), 127, device="cuda", dtype=torch.int8), torch.full((rows, 2), 120, device="cuda", dtype=torch.uint8)
+    scales[0, 1] = 255
+    codes[0, 40], codes[0, 41] = 0, -5
+    p = nn.Packed8(codes, scales, 64)
+    got = nn.unpack8(p, dt)
+    assert torch.isnan(got[0, 32:]).all() and torch.isfinite(got[0, :32]).all() and torch.isfinite(got[1:]).all()
+    y = nn.linear(p, torch.ones(9, 64, device="cuda", dtype=dt))
+    assert torch.isnan(y[0]).all() and torch.isfinite(y[1:]).all()
+    dx, dw, db = nn.linear_backward(torch.ones(rows, 64, device="cuda", dtype=dt), p, torch.ones(64, 64, device="cuda", dtype=dt), act="silu", z=p)
+    assert torch.isnan(db[32:]).all() and torch.isfinite(db[:32]).all() and torch.isnan(dw[:, 32:]).all() and torch.isfinite(dw[:32, :32]).all()
+    narrow = nn.Packed8(codes[:1, :32].contiguous(), scales[:1, 1:].contiguous(), 6)
+    assert torch.isnan(nn.linear(narrow, torch.ones(1, 6, device="cuda", dtype=dt))).all()

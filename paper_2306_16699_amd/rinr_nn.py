@@ -159,11 +159,15 @@ class _There(_Here):
         if dev.index != torch.cuda.current_device():
             self._guard = torch.cuda.device(dev)
             self._guard.__enter__()
-        super().__init__(dev, rinr._stream_ptr(stream))
-        if stream is not None:
-            s = stream if isinstance(stream, torch.cuda.Stream) else \
-                (torch.cuda.ExternalStream(self.ptr, device=dev) if self.ptr else torch.cuda.default_stream(dev))
-            self._side = torch.cuda.stream(s)
+        try:
+            super().__init__(dev, rinr._stream_ptr(stream))
+            if stream is not None:
+                s = stream if isinstance(stream, torch.cuda.Stream) else \
+                    (torch.cuda.ExternalStream(self.ptr, device=dev) if self.ptr else torch.cuda.default_stream(dev))
+                self._side = torch.cuda.stream(s)
+        except BaseException:
+            self.close()                                               # what is no stream leaves the caller on its GPU
+            raise
 
     def empty(self, like, shape, dtype):
         if self._side is None:

@@ -194,3 +194,24 @@ def test_a_packed_matrix_has_the_shape_of_its_rows():
     for name in ("shape", "rows", "cols", "ld", "device", "codes", "scales"):
         with pytest.raises(AttributeError):
             setattr(p, name, getattr(p, name))
+
+
+def test_what_is_no_stream_leaves_the_caller_on_its_gpu(monkeypatch):
+    at = [0]
+
+    class Guard:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def __enter__(self):
+            self.before, at[0] = at[0], self.dev.index
+
+        def __exit__(self, *_):
+            at[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: at[0])
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    for stream in ("side", object(), 1.5):
+        with pytest.raises(AttributeError):
+            rinr_nn._on(torch.device("cuda:1"), stream)
+        assert at[0] == 0

@@ -3,7 +3,8 @@
 Argument marshalling only; every operator runs in the HIP kernels of librinr.so.  PyTorch owns memory and streams.  Activations are matrices
 whose last dimension has unit stride (any leading dimensions that lie evenly apart); weights are [n_out, n_in]; bias and gain are
 float32.  `stream`: a torch stream, an integer handle (0: the GPU's default stream) or None for the current one; outputs and scratch
-memory come from the stream that works on them, and what the caller passes has to be ready there.
+memory come from the stream that works on them.  What the caller passes has to be ready there; it may be dropped at once, as its memory is not handed
+on before that stream has done with it.
 """
 from __future__ import annotations
 
@@ -151,11 +152,11 @@ class _Here:
 
 
 class _There(_Here):
-    """A call on another GPU or stream than the current one: outputs and scratch memory are of that stream."""
-    __slots__ = ("_guard", "_side")
+    """A call on another GPU or stream than the current one: outputs and scratch memory are of that stream, and inputs are held until it has done with them."""
+    __slots__ = ("_guard", "_side", "_stream")
 
     def __init__(self, dev, stream):
-        self._guard = self._side = None
+        self._guard = self._side = self._stream = None
         if dev.index != torch.cuda.current_device():
             self._guard = torch.cuda.device(dev)
             self._guard.__enter__()
@@ -164,7 +165,7 @@ class _There(_Here):
             if stream is not None:
                 s = stream if isinstance(stream, torch.cuda.Stream) else \
                     (torch.cuda.ExternalStream(self.ptr, device=dev) if self.ptr else torch.cuda.default_stream(dev))
-                self._side = torch.cuda.stream(s)
+                self._side, self._stream = torch.cuda.stream(s), s
         except BaseException:
             self.close()                                               # what is no stream leaves the caller on its GPU
             raise
@@ -177,6 +178,13 @@ class _There(_Here):
             t = torch.empty(shape, dtype=dtype, device=self.dev)
         t.record_stream(here)                                          # where the caller goes on with it
         return t
+
+    def hold(self, *inputs):
+        for t in inputs:
+            if type(t) is Packed8:
+                self.hold(*((t._codes, t._scales) if t._both is None else (t._both,)))
+            elif t is not None:
+                t.record_stream(self._stream)
 
     def close(self):
         if self._guard is not None:
@@ -272,6 +280,8 @@ def linear(x, w, bias=None, act: str = "none", w0: float = 30.0, residual=None, 
         py, _, _, ldy = _alike(out, dtype, shape, dev, "rinr_linear out")
     on = _on(dev, stream)
     try:
+        if stream is not None:
+            on.hold(x, w, bias, residual, out)
         if out is None:
             out = on.empty(w, shape, dtype)
             py, ldy = out.data_ptr(), n_out
@@ -312,6 +322,8 @@ def linear_backward(dy, x, w, act: str = "none", w0: float = 30.0, z=None, x_act
             _fail(f"{what}: z has {zr} x {zc} on {z.device}, dy {rows} x {n_out} on {dev}")
     on = _on(dev, stream)
     try:
+        if stream is not None:
+            on.hold(dy, x, w, z)
         dx = on.empty(w, x.shape, dtype) if need_dx else None
         dw = on.empty(w, (n_out, n_in), dtype) if need_dw else None
         db = on.empty(w, (n_out,), torch.float32) if need_db else None
@@ -337,6 +349,8 @@ def rms_norm(x, gain, eps: float = 1e-6, residual=None, packed: bool = False, st
         pr, _, _, ldr = _alike(residual, dtype, shape, dev, "rinr_rms_norm residual")
     on = _on(dev, stream)
     try:
+        if stream is not None:
+            on.hold(x, gain, residual)
         h = x if residual is None else on.empty(x, shape, dtype)
         if packed:
             y = Packed8._new(on, x, rows, cols, tuple(shape))
@@ -366,6 +380,8 @@ def rms_norm_backward(dy, h, gain, eps: float = 1e-6, dres=None, need_dgain: boo
         pd, _, _, ldd = _alike(dres, dtype, shape, dev, "rinr_rms_norm_backward dres")
     on = _on(dev, stream)
     try:
+        if stream is not None:
+            on.hold(dy, h, gain, dres)
         dh = on.empty(h, shape, dtype)
         dgain = on.empty(h, (cols,), torch.float32) if need_dgain else None
         need = L.rinr_rms_norm_backward_workspace_bytes(rows, cols) if need_dgain else 0
@@ -385,6 +401,8 @@ def pack8(x, stream=None) -> Packed8:
     px, rows, cols, ldx = _mat(x, what)
     on = _on(x.device, stream)
     try:
+        if stream is not None:
+            on.hold(x)
         p = Packed8._new(on, x, rows, cols, tuple(x.shape))
         pc, ps = p._pointers()
         rinr._check(L.rinr_pack8(rows, cols, px, ldx, TYPES[x.dtype], pc, p.ld, ps, on.ptr), what)
@@ -402,6 +420,8 @@ def unpack8(p: Packed8, dtype=torch.bfloat16, act: str = "none", w0: float = 30.
     pc, ps = p._pointers()
     on = _on(p.device, stream)
     try:
+        if stream is not None:
+            on.hold(p)
         x = on.empty(p._codes if p._both is None else p._both, p.shape, dtype)
         rinr._check(L.rinr_unpack8(p.rows, p.cols, pc, p.ld, ps, ka, w0, x.data_ptr(), p.cols, TYPES[dtype], on.ptr), what)
     finally:

@@ -220,3 +220,52 @@ def test_a_block_that_stands_for_nan_is_nan_whatever_its_codes(rows, dtype):
     assert torch.isnan(db[32:]).all() and torch.isfinite(db[:32]).all() and torch.isnan(dw[:, 32:]).all() and torch.isfinite(dw[:32, :32]).all()
     narrow = nn.Packed8(codes[:1, :32].contiguous(), scales[:1, 1:].contiguous(), 6)
     assert torch.isnan(nn.linear(narrow, torch.ones(1, 6, device="cuda", dtype=dt))).all()
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("call", ["linear", "linear_backward", "rms_norm", "rms_norm_backward", "pack8", "unpack8"])
+def test_inputs_are_held_for_the_stream_that_works_on_them(call, handle):
+    """A caller may drop what it passed as soon as the call returns: while the other stream is still busy, its memory goes to nobody else."""
+    side, g = torch.cuda.Stream(), gen(4)
+    n = 96
+
+    def matrix():
+        return torch.randn(n, n, generator=g, device="cuda").to(torch.bfloat16)
+
+    def packed():
+        p = nn.pack8(matrix())
+        return nn.Packed8(p.codes.clone(), p.scales.clone(), n)
+
+    def vector():
+        return torch.randn(n, generator=g, device="cuda")
+
+    given, kw = {"linear": ((packed(), matrix(), vector()), dict(residual=matrix(), out=matrix(), keep_z="packed", act="gelu")),
+                 "linear_backward": ((matrix(), matrix(), matrix()), dict(act="gelu", z=packed(), x_act="silu")),
+                 "rms_norm": ((matrix(), vector()), dict(residual=matrix())), "rms_norm_backward": ((matrix(), matrix(), vector()), dict(dres=matrix())),
+                 "pack8": ((matrix(),), {}), "unpack8": ((nn.pack8(matrix()),), {})}[call]
+    op = getattr(nn, call)
+    want = op(*given, **{k: v.clone() if k == "out" else v for k, v in kw.items()})
+    tensors = [t for v in (*given, *kw.values()) for t in ((v._codes, v._scales, v._both) if isinstance(v, nn.Packed8) else (v,)) if isinstance(t, torch.Tensor)]
+    torch.cuda.synchronize()
+    held = {t.data_ptr(): t.untyped_storage().nbytes() for t in tensors}
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)                                 # some 50 ms
+    got = op(*given, **kw, stream=side.cuda_stream if handle else side)
+    ended = torch.cuda.Event()
+    ended.record(side)
+    del given, kw, tensors
+    others = [torch.full((size,), 0x7f, device="cuda", dtype=torch.uint8) for size in held.values() for _ in range(3)]
+    busy = not ended.query()
+    assert not held.keys() & {t.data_ptr() for t in others}
+    torch.cuda.synchronize()
+    assert busy                                                        # else nothing has been tested
+
+    def flat(v):
+        for t in v if isinstance(v, tuple) else (v,):
+            if isinstance(t, nn.Packed8):
+                yield from (t.codes, t.scales)
+            elif t is not None:
+                yield t
+
+    for a, b in zip(flat(got), flat(want)):
+        assert torch.equal(a, b)

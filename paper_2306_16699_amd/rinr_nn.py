@@ -5,6 +5,9 @@ whose last dimension has unit stride (any leading dimensions that lie evenly apa
 float32.  `stream`: a torch stream, an integer handle (0: the GPU's default stream) or None for the current one; outputs and scratch
 memory come from the stream that works on them.  What the caller passes has to be ready there; it may be dropped at once, as its memory is not handed
 on before that stream has done with it.
+
+No operator keeps a graph for automatic differentiation: while gradients are being recorded, tensors that require them are refused.  Under torch.no_grad(),
+and so inside the forward and backward of a torch.autograd.Function, whose gradients are those of the `_backward` operators, they are taken.
 """
 from __future__ import annotations
 
@@ -116,8 +119,15 @@ def _fail(what: str):
     raise rinr.RinrError(rinr.E_ARG, what)
 
 
+def _no_graph(what: str):
+    if torch.is_grad_enabled():
+        _fail(what + ": keeps no graph for tensors that require gradients; torch.no_grad(), or a torch.autograd.Function around it and its backward operator")
+
+
 def _mat(t, what: str):
     """(pointer, rows, columns, distance between rows) of a tensor's rows."""
+    if t.requires_grad:
+        _no_graph(what)
     shape = t.shape
     if len(shape) != 2:
         if not shape or shape[-1] < 1:
@@ -231,6 +241,8 @@ def _operand(x, dtype, dt: int, what: str):
 
 
 def _vector(v, n: int, dev, what: str):
+    if v.requires_grad:
+        _no_graph(what)
     if v.dtype != torch.float32 or v.shape != (n,) or not v.is_contiguous() or v.device != dev:
         _fail(f"{what}: a float32 vector of {n} on {dev}")
     return v.data_ptr()

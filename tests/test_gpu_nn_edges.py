@@ -269,3 +269,42 @@ def test_inputs_are_held_for_the_stream_that_works_on_them(call, handle):
 
     for a, b in zip(flat(got), flat(want)):
         assert torch.equal(a, b)
+
+
+def test_every_tensor_that_requires_gradients_is_refused_while_these_are_recorded():
+    def matrix(n=8):
+        return torch.randn(8, n, device="cuda")
+
+    calls = [(lambda x, w, b, r: nn.linear(x, w, b, residual=r), lambda: [matrix(), matrix(), matrix()[0], matrix()]),
+             (lambda dy, x, w, z: nn.linear_backward(dy, x, w, act="gelu", z=z), lambda: [matrix() for _ in range(4)]),
+             (lambda x, g, r: nn.rms_norm(x, g, residual=r), lambda: [matrix(), matrix()[0], matrix()]),
+             (lambda dy, h, g, d: nn.rms_norm_backward(dy, h, g, dres=d), lambda: [matrix(), matrix(), matrix()[0], matrix()]),
+             (lambda x: nn.pack8(x), lambda: [matrix()])]
+    for call, make in calls:
+        for k in range(len(make())):
+            given = make()
+            given[k] = given[k].clone().requires_grad_()
+            with pytest.raises(rinr.RinrError, match="no graph"):
+                call(*given)
+            with torch.no_grad():
+                call(*given)
+
+    class Layer(torch.autograd.Function):
+        """The way to a graph: the operators' own gradients."""
+        @staticmethod
+        def forward(ctx, x, w, b):
+            y, z = nn.linear(x, w, b, act="gelu", keep_z="tensor")
+            ctx.save_for_backward(x, w, z)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, w, z = ctx.saved_tensors
+            return nn.linear_backward(dy.contiguous(), x, w, act="gelu", z=z)
+
+    x, w, b = (t.requires_grad_() for t in (matrix(), matrix(), matrix()[0].clone()))
+    Layer.apply(x, w, b).sum().backward()
+    x64, w64, b64 = (t.detach().double().cpu().requires_grad_() for t in (x, w, b))
+    torch.nn.functional.gelu(x64 @ w64.t() + b64).sum().backward()
+    for a, c in ((x, x64), (w, w64), (b, b64)):                        # some 30 operations of 2^-22 of a value below 30
+        assert float((a.grad.double().cpu() - c.grad).abs().max()) < 30 * 30 * 2.0 ** -22

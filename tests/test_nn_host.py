@@ -215,3 +215,27 @@ def test_what_is_no_stream_leaves_the_caller_on_its_gpu(monkeypatch):
         with pytest.raises(AttributeError):
             rinr_nn._on(torch.device("cuda:1"), stream)
         assert at[0] == 0
+
+
+def _refusal(call):
+    with pytest.raises(rinr.RinrError) as e:
+        call()
+    assert e.value.code == rinr.E_ARG
+    return str(e.value)
+
+
+def test_tensors_that_require_gradients_are_refused_while_these_are_recorded():
+    """A result without a graph would leave its inputs without gradients, and say nothing."""
+    x, v = torch.zeros(4, 8, requires_grad=True), torch.zeros(8, requires_grad=True)
+    assert "no graph" in _refusal(lambda: rinr_nn._mat(x, "x")) and "no graph" in _refusal(lambda: rinr_nn._vector(v, 8, v.device, "bias"))
+    assert "no graph" in _refusal(lambda: rinr_nn.pack8(x)) and "no graph" in _refusal(lambda: rinr_nn.rms_norm(x, v))
+    with torch.no_grad():
+        assert rinr_nn._vector(v, 8, v.device, "bias") == v.data_ptr()
+        assert "on the GPU" in _refusal(lambda: rinr_nn.pack8(x))      # for where it is, not for its gradients
+
+    class Packed(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return rinr_nn.pack8(x)
+
+    assert "on the GPU" in _refusal(lambda: Packed.apply(x))

@@ -8,7 +8,8 @@
  *
  * Same conventions as rinr.h: plain C ABI, 0 or a negative RINR_E_* code, every pointer of this file is a device pointer, the caller
  * owns every buffer, nothing is allocated and nothing is waited for: kernels go to `stream` in order.  All matrices are
- * row-major with unit stride between columns; ld_* is the distance between rows in elements.
+ * row-major with unit stride between columns; ld_* is the distance between rows in elements.  What a call writes shares no memory with what it
+ * reads or with another result, but where a field says so.
  *
  * Types: RINR_T_BF16, _F16 and _F32 matrices, aligned to their element.  A packed matrix (RINR_T_PACKED8) holds 8-bit codes:
  * every 32 columns of a row (a block; the last may be shorter) share one scale byte e, the value is code * 2^(e - 127), codes are
@@ -65,7 +66,8 @@ typedef struct {
  * products' k, and x as dtype, where a large product takes a packed one. */
 size_t rinr_linear_workspace_bytes(const rinr_linear_args *a);
 /* workspace: 16-byte aligned device memory, in use until the call's kernels have run.  RINR_E_NULL / RINR_E_ARG (sizes, strides,
- * types) / RINR_E_SIZE (workspace_bytes less than that) / RINR_E_ALIGN / RINR_E_HIP.  rows = 0 does nothing. */
+ * types;
+ * y or z on top of x or w, y on part of the residual) / RINR_E_SIZE (workspace_bytes less than that) / RINR_E_ALIGN / RINR_E_HIP.  rows = 0 does nothing. */
 int rinr_linear(const rinr_linear_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Gradients of y = act(z), z = x w' + bias, given dy (the residual's gradient is dy itself):

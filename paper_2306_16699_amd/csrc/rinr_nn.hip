@@ -35,6 +35,14 @@ int check_mat(const void *p, int64_t ld, const uint8_t *scales, int type, int64_
     if (ld < cols) return RINR_E_ARG;
     return aligned(p, size_of(type)) ? RINR_OK : RINR_E_ALIGN;
 }
+// Whether two matrices of rows of `a_row`, `b_row` bytes share memory: their spans do, and rows equally far apart do not lie beside each other
+bool overlap(const void *a, int64_t a_rows, int64_t a_row, int64_t a_ld, const void *b, int64_t b_rows, int64_t b_row, int64_t b_ld) {
+    const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+    if (pa + (uintptr_t)((a_rows - 1) * a_ld + a_row) <= pb || pb + (uintptr_t)((b_rows - 1) * b_ld + b_row) <= pa) return false;
+    if (a_ld != b_ld) return true;
+    const int64_t on = pb >= pa ? (int64_t)((pb - pa) % (uintptr_t)a_ld) : (a_ld - (int64_t)((pa - pb) % (uintptr_t)a_ld)) % a_ld;    // b's rows begin there in a's
+    return on < a_row || on + b_row > a_ld;
+}
 #define NN_CHECK(call) do { const int rc_ = (call); if (rc_) return rc_; } while (0)
 
 bool good_act(int act, float w0) { return act >= RINR_ACT_NONE && act <= RINR_ACT_SINE && (act != RINR_ACT_SINE || (w0 - w0 == 0.0f)); }
@@ -212,6 +220,18 @@ int check_linear(const rinr_linear_args *a) {
     return aligned(a->bias, 4) ? RINR_OK : RINR_E_ALIGN;
 }
 
+// Workgroups read x and w while others write: y and z lie apart from both.  The residual is read where y is written, by the same thread.
+int check_linear_apart(const rinr_linear_args *a) {
+    const int64_t el = (int64_t)size_of(a->dtype), x_el = a->x_type == RINR_T_PACKED8 ? 1 : el, z_el = a->z_type == RINR_T_PACKED8 ? 1 : el;
+    const auto touches = [&](const void *p, int64_t el_p, int64_t ld) {
+        return overlap(p, a->rows, a->n_out * el_p, ld * el_p, a->x, a->rows, a->n_in * x_el, a->ld_x * x_el) ||
+               overlap(p, a->rows, a->n_out * el_p, ld * el_p, a->w, a->n_out, a->n_in * el, a->ld_w * el);
+    };
+    if (touches(a->y, el, a->ld_y) || (a->z_type != RINR_T_NONE && touches(a->z, z_el, a->ld_z))) return RINR_E_ARG;
+    const bool in_place = a->residual == a->y && (a->ld_residual == a->ld_y || a->rows == 1);
+    return a->residual && !in_place && overlap(a->y, a->rows, a->n_out * el, a->ld_y * el, a->residual, a->rows, a->n_out * el, a->ld_residual * el) ? RINR_E_ARG : RINR_OK;
+}
+
 int check_linear_grad(const rinr_linear_grad_args *a) {
     if (!a) return RINR_E_NULL;
     if (!good_sizes(a->rows, a->n_in, a->n_out) || !is_float_type(a->dtype) || !good_act(a->act, a->w0) || !good_act(a->x_act, a->w0)) return RINR_E_ARG;
@@ -370,6 +390,7 @@ extern "C" size_t rinr_linear_workspace_bytes(const rinr_linear_args *a) { retur
 extern "C" int rinr_linear(const rinr_linear_args *a, void *workspace, size_t workspace_bytes, void *stream) {
     NN_CHECK(check_linear(a));
     if (a->rows == 0) return RINR_OK;
+    NN_CHECK(check_linear_apart(a));
     const LinearPlan l = linear_plan(a, (char *)workspace);
     if (l.bytes && !workspace) return RINR_E_NULL;
     if (workspace_bytes < l.bytes) return RINR_E_SIZE;

@@ -308,3 +308,21 @@ def test_every_tensor_that_requires_gradients_is_refused_while_these_are_recorde
     torch.nn.functional.gelu(x64 @ w64.t() + b64).sum().backward()
     for a, c in ((x, x64), (w, w64), (b, b64)):                        # some 30 operations of 2^-22 of a value below 30
         assert float((a.grad.double().cpu() - c.grad).abs().max()) < 30 * 30 * 2.0 ** -22
+
+
+def test_results_beside_what_is_read_are_taken_and_on_top_of_it_refused():
+    g = gen(8)
+    w = torch.randn(48, 48, generator=g, device="cuda").to(torch.bfloat16)
+    both = torch.randn(20, 96, generator=g, device="cuda").to(torch.bfloat16)
+    x, out = both[:, :48], both[:, 48:]                                # rows of one beside rows of the other
+    want = nn.linear(x.contiguous(), w)
+    assert nn.linear(x, w, out=out) is out and torch.equal(out, want)
+    x, out = both[:, 48:], both[:, :48]
+    want = nn.linear(x.contiguous(), w)
+    assert torch.equal(nn.linear(x, w, out=out), want)
+    x = torch.randn(20, 48, generator=g, device="cuda").to(torch.bfloat16)
+    for bad in (dict(out=x), dict(out=w[:20]), dict(out=both[:, 1:49], residual=both[:, :48]), dict(out=both.view(-1)[:960].view(20, 48), residual=both[:, :48])):
+        with pytest.raises(rinr.RinrError):
+            nn.linear(x, w, **bad)
+    with pytest.raises(rinr.RinrError):
+        nn.linear(both[:, :48], w, out=both[:, 47:95])

@@ -239,3 +239,14 @@ def test_tensors_that_require_gradients_are_refused_while_these_are_recorded():
             return rinr_nn.pack8(x)
 
     assert "on the GPU" in _refusal(lambda: Packed.apply(x))
+
+
+@pytest.mark.parametrize("change", [dict(), dict(y=4096 + 2), dict(y=4096 + 3 * 16 + 14), dict(y=1 << 20, z=4096, ld_z=8, z_type=1), dict(y=1 << 20, z=1 << 21, ld_z=8, z_type=1, w=1 << 21),
+                                    dict(y=1 << 20, w=(1 << 20) + 14), dict(y=1 << 20, residual=(1 << 20) + 2, ld_residual=8), dict(y=1 << 20, residual=1 << 20, ld_residual=16),
+                                    dict(y=4096 + 14, ld_y=16, ld_x=16), dict(y=4096 + 18, ld_y=16, ld_x=16), dict(x=4096 + 18, y=4096, ld_y=16, ld_x=16),
+                                    dict(x=4096, x_type=4, ld_x=32, x_scales=1 << 22, y=4096 + 100), dict(y=4096 + 16, ld_y=9, ld_x=16)], ids=str)
+def test_linear_refuses_results_on_top_of_what_it_reads(change):
+    """Checked before anything else is done with the pointers: these never reach a kernel."""
+    args = dict(w=1 << 30)
+    args.update(change)
+    assert rinr_nn.lib().rinr_linear(linear_args(**args), None, 0, None) == rinr.E_ARG

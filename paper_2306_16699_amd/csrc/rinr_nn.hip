@@ -177,7 +177,7 @@ template <class T> void launch_join(const float *part, const Plan &p, int64_t nq
 
 template <class T> void launch_tiny(int what, bool x_packed, const GemmArgs &a, hipStream_t st) {
     const int64_t tasks = div_up(a.P.n, kBlock8) * 4 * a.Q.n;
-    hipLaunchKernelGGL(tiny_kernel<T>, dim3((uint32_t)div_up(tasks, 256)), dim3(256), 0, st, a, tasks, what != kForward, what == kGradW, x_packed && what == kGradW,
+    hipLaunchKernelGGL(tiny_kernel<T>, grid_of(div_up(tasks, 256)), dim3(256), 0, st, a, tasks, what != kForward, what == kGradW, x_packed && what == kGradW,
                        x_packed && what == kForward);
 }
 #define NN_BY_TYPE(dtype, call, ...) \
@@ -203,7 +203,7 @@ int product(int dtype, int what, bool x_packed, const Plan &p, const Side &P, co
 
 bool good_sizes(int64_t rows, int64_t n_in, int64_t n_out) {
     return rows >= 0 && rows <= kMaxRows && n_in >= 1 && n_in <= RINR_NN_MAX_FEATURES && n_out >= 1 && n_out <= RINR_NN_MAX_FEATURES &&
-           div_up(rows, kTile) * div_up(std::max(n_in, n_out), kTile) <= INT32_MAX;
+           div_up(rows, kTile) * div_up(std::max(n_in, n_out), kTile) * kTileThreads <= UINT32_MAX;      // threads of a launch
 }
 
 int check_linear(const rinr_linear_args *a) {
@@ -307,19 +307,19 @@ void launch_sum_parts(const float *part, int64_t n, int64_t cols, float *out, hi
     hipLaunchKernelGGL(sum_parts_kernel, dim3((uint32_t)div_up(cols, 32)), dim3(1024), 0, st, part, n, cols, out);
 }
 template <class T, bool LOW> void launch_unpack(int64_t rows, int64_t cols, const void *codes, int64_t ld, const uint8_t *scales, const Act &act, void *x, int64_t ld_x, hipStream_t st) {
-    hipLaunchKernelGGL((unpack_kernel<T, LOW>), dim3((uint32_t)div_up(rows * div_up(cols, 8), 256)), dim3(256), 0, st, rows, (int)cols, (const int8_t *)codes, ld, scales, act, (T *)x,
+    hipLaunchKernelGGL((unpack_kernel<T, LOW>), grid_of(div_up(rows * div_up(cols, 8), 256)), dim3(256), 0, st, rows, (int)cols, (const int8_t *)codes, ld, scales, act, (T *)x,
                        ld_x, rows * cols * (int64_t)sizeof(T) > kPastL2);
 }
 template <class T> void launch_values(int64_t rows, int64_t cols, const void *codes, int64_t ld, const uint8_t *scales, const Act &act, void *x, int64_t ld_x, hipStream_t st) {
     launch_unpack<T, false>(rows, cols, codes, ld, scales, act, x, ld_x, st);
 }
-template <class T> void launch_pack(uint32_t blocks, int64_t rows, int64_t cols, const void *x, int64_t ld_x, void *codes, int64_t ld, uint8_t *scales, hipStream_t st) {
-    hipLaunchKernelGGL(pack_kernel<T>, dim3(blocks), dim3(256), 0, st, rows, (int)cols, (const T *)x, ld_x, (int8_t *)codes, ld, scales, rows * cols > kPastL2);
+template <class T> void launch_pack(int64_t rows, int64_t cols, const void *x, int64_t ld_x, void *codes, int64_t ld, uint8_t *scales, hipStream_t st) {
+    hipLaunchKernelGGL(pack_kernel<T>, grid_of(div_up(rows * div_up(cols, kBlock8) * 4, 256)), dim3(256), 0, st, rows, (int)cols, (const T *)x, ld_x, (int8_t *)codes, ld, scales, rows * cols > kPastL2);
 }
 template <class T, bool LOW> void launch_act_parts(int64_t rows, int64_t cols, const void *z, int64_t ld, const uint8_t *scales, bool packed, const Act &act, void *x, int64_t ld_x,
                                                    hipStream_t st) {
     if (packed) launch_unpack<T, LOW>(rows, cols, z, ld, scales, act, x, ld_x, st);
-    else hipLaunchKernelGGL((act_kernel<T, LOW>), dim3((uint32_t)div_up(rows * div_up(cols, 8), 256)), dim3(256), 0, st, rows, (int)cols, (const T *)z, ld, act, (T *)x, ld_x,
+    else hipLaunchKernelGGL((act_kernel<T, LOW>), grid_of(div_up(rows * div_up(cols, 8), 256)), dim3(256), 0, st, rows, (int)cols, (const T *)z, ld, act, (T *)x, ld_x,
                             rows * cols * (int64_t)sizeof(T) > kPastL2);
 }
 // two_parts: of 16-bit types only
@@ -339,12 +339,12 @@ int64_t norm_grad_blocks(int64_t rows, int64_t cols) {
 }
 
 template <class T, bool PACKED> void launch_norm(const NormArgs &a, hipStream_t st) {
-    const uint32_t grid = (uint32_t)div_up(a.rows, norm_slots(a.cols));
-    if (a.cols <= 512) hipLaunchKernelGGL((norm_kernel<T, 64, 1, PACKED>), dim3(grid), dim3(256), 0, st, a);
-    else if (a.cols <= 1024) hipLaunchKernelGGL((norm_kernel<T, 64, 2, PACKED>), dim3(grid), dim3(256), 0, st, a);
-    else if (a.cols <= 4096) hipLaunchKernelGGL((norm_kernel<T, 256, 2, PACKED>), dim3(grid), dim3(256), 0, st, a);
-    else if (a.cols <= 8192) hipLaunchKernelGGL((norm_kernel<T, 256, 4, PACKED>), dim3(grid), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((norm_kernel<T, 1024, 4, PACKED>), dim3(grid), dim3(1024), 0, st, a);
+    const dim3 grid = grid_of(div_up(a.rows, norm_slots(a.cols)));
+    if (a.cols <= 512) hipLaunchKernelGGL((norm_kernel<T, 64, 1, PACKED>), grid, dim3(256), 0, st, a);
+    else if (a.cols <= 1024) hipLaunchKernelGGL((norm_kernel<T, 64, 2, PACKED>), grid, dim3(256), 0, st, a);
+    else if (a.cols <= 4096) hipLaunchKernelGGL((norm_kernel<T, 256, 2, PACKED>), grid, dim3(256), 0, st, a);
+    else if (a.cols <= 8192) hipLaunchKernelGGL((norm_kernel<T, 256, 4, PACKED>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((norm_kernel<T, 1024, 4, PACKED>), grid, dim3(1024), 0, st, a);
 }
 template <class T> void launch_norm_grad(const NormGradArgs &a, hipStream_t st) {
     const uint32_t grid = (uint32_t)norm_grad_blocks(a.rows, a.cols);
@@ -532,9 +532,8 @@ extern "C" int rinr_pack8(int64_t rows, int64_t cols, const void *x, int64_t ld_
     if (rows == 0) return RINR_OK;
     NN_CHECK(check_mat(x, ld_x, nullptr, dtype, cols));
     NN_CHECK(check_mat(codes, ld, scales, RINR_T_PACKED8, cols));
-    const int64_t blocks = div_up(rows * div_up(cols, kBlock8) * 4, 256);
-    if (blocks > INT32_MAX) return RINR_E_UNSUPPORTED;
-    NN_BY_TYPE(dtype, launch_pack, (uint32_t)blocks, rows, cols, x, ld_x, codes, ld, scales, (hipStream_t)stream);
+    if (div_up(rows * div_up(cols, kBlock8) * 4, 256) > INT32_MAX) return RINR_E_UNSUPPORTED;
+    NN_BY_TYPE(dtype, launch_pack, rows, cols, x, ld_x, codes, ld, scales, (hipStream_t)stream);
     return launched();
 }
 

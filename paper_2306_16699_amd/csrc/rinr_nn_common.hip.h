@@ -21,6 +21,12 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));          // of 16-bit values: at any of their addresses
 constexpr int kBlock8 = 32;                   // columns that share a scale
 
+// Workgroups of any number: a launch counts its threads along x in 32 bits, so more than kAcross of up to 1024 threads go on along y.  The last of these rows
+// of workgroups may be longer than what is left.
+constexpr int64_t kAcross = 1 << 21;
+inline dim3 grid_of(int64_t blocks) { return dim3((uint32_t)(blocks < kAcross ? blocks : kAcross), (uint32_t)((blocks + kAcross - 1) / kAcross)); }
+__device__ __forceinline__ int64_t block_of() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 template <class T> __device__ __forceinline__ T from_float(float v) { return (T)v; }
 
 // At both ends of a branch whose accesses differ from the other branch's in nothing but where they are to be cached: else the compiler makes one access,

@@ -725,7 +725,7 @@ template <class T> struct TinySide {
     }
 };
 template <class T> __global__ __launch_bounds__(256) void tiny_kernel(const GemmArgs a, int64_t tasks, bool kp, bool kq, bool p_packed, bool q_packed) {
-    const int64_t per_row = (a.P.n + kBlock8 - 1) / kBlock8 * 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t per_row = (a.P.n + kBlock8 - 1) / kBlock8 * 4, at = block_of() * 256 + threadIdx.x;
     if (at >= tasks) return;                                                     // of all 4 threads of a block
     const int64_t q = at / per_row, p = (at - q * per_row) * 8;
     const int have = (int)(a.P.n - p < 8 ? a.P.n - p : 8);

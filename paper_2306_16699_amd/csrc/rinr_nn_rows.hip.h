@@ -54,8 +54,8 @@ template <class T, int TPR, int NV, bool PACKED> __global__ __launch_bounds__(TP
     constexpr int THREADS = TPR < 256 ? 256 : TPR, SLOTS = THREADS / TPR;
     __shared__ float scratch[2 * THREADS / 64];
     const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * SLOTS + threadIdx.x / TPR;
-    if (row >= a.rows) return;                                                   // of a whole wavefront; rows of workgroups are always there
+    const int64_t row = block_of() * SLOTS + threadIdx.x / TPR;
+    if (row >= a.rows) return;                                                   // of a whole wavefront, or a whole workgroup
     float h[NV][8], ss = 0.0f, none = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(const float *part, int6
 // (5.6 TB/s), back 59 (6.8), back through GELU 84 (its 17 vector instructions a value).
 template <class T> __global__ __launch_bounds__(256) void pack_kernel(int64_t rows, int cols, const T *x, int64_t ld_x, int8_t *codes, int64_t ld, uint8_t *scales, bool past) {
     const int64_t per_row = (cols + kBlock8 - 1) / kBlock8 * 4;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t at = block_of() * 256 + threadIdx.x;
     const int64_t row = at / per_row;
     const int col = (int)(at - row * per_row) * 8;
     float v[8] = {};
@@ -218,7 +218,7 @@ template <class T, bool LOW> __device__ __forceinline__ void store_act(T *x, int
 template <class T, bool LOW> __global__ __launch_bounds__(256) void unpack_kernel(int64_t rows, int cols, const int8_t *codes, int64_t ld, const uint8_t *scales, const Act act, T *x,
                                                                        int64_t ld_x, bool past) {
     const int64_t per_row = (cols + 7) / 8;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t at = block_of() * 256 + threadIdx.x;
     const int64_t row = at / per_row;
     if (row >= rows) return;
     const int col = (int)(at - row * per_row) * 8;
@@ -232,7 +232,7 @@ template <class T, bool LOW> __global__ __launch_bounds__(256) void unpack_kerne
 
 template <class T, bool LOW> __global__ __launch_bounds__(256) void act_kernel(int64_t rows, int cols, const T *z, int64_t ld_z, const Act act, T *x, int64_t ld_x, bool past) {
     const int64_t per_row = (cols + 7) / 8;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t at = block_of() * 256 + threadIdx.x;
     const int64_t row = at / per_row;
     if (row >= rows) return;
     const int col = (int)(at - row * per_row) * 8;

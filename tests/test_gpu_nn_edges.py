@@ -326,3 +326,32 @@ def test_results_beside_what_is_read_are_taken_and_on_top_of_it_refused():
             nn.linear(x, w, **bad)
     with pytest.raises(rinr.RinrError):
         nn.linear(both[:, :48], w, out=both[:, 47:95])
+
+
+def test_more_threads_than_a_launch_counts_along_x():
+    """2^32 threads and more: rows of a norm, groups of 8 columns of checkpoints, results of a product of few values."""
+    if torch.cuda.mem_get_info()[0] < 130 << 30:
+        pytest.skip("130 GB of GPU memory")
+    g = gen(12)
+    rows, half = (1 << 26) + 5, (1 << 25) + 1
+    x, gain = torch.randint(-8, 9, (rows, 3), generator=g, device="cuda", dtype=torch.int8).to(torch.bfloat16), torch.rand(3, generator=g, device="cuda")
+    y, _ = nn.rms_norm(x, gain)
+    assert torch.equal(y[:half], nn.rms_norm(x[:half], gain)[0]) and torch.equal(y[half:], nn.rms_norm(x[half:], gain)[0])
+    del x, y
+    rows = (1 << 30) + 7
+    x = torch.randint(-127, 128, (rows, 1), generator=g, device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    x[-1] = 77.0
+    p = nn.pack8(x)
+    assert torch.equal(nn.unpack8(p), x)
+    w = torch.tensor([[2.0], [-1.0], [0.5]], device="cuda", dtype=torch.bfloat16)
+    y = nn.linear(x, w)
+    for k in range(3):
+        assert torch.equal(y[:, k], (x[:, 0].float() * float(w[k])).to(torch.bfloat16)), k
+    del x, p, y
+    codes = torch.zeros((1 << 20) + 1, 1 << 15, device="cuda", dtype=torch.int8)
+    scales = torch.full(((1 << 20) + 1, 1 << 10), 127, device="cuda", dtype=torch.uint8)
+    codes[-1], codes[0] = 5, -3
+    x = nn.unpack8(nn.Packed8(codes, scales, 1 << 15))
+    assert bool((x[-1] == 5).all()) and bool((x[0] == -3).all()) and not x[1:1000].any() and not x[-1000:-1].any()
+    del codes, scales, x
+    torch.cuda.empty_cache()

@@ -1,10 +1,12 @@
 """Operators for networks on decoded batches at the edges of their range on the GPU: infinities, the largest numbers, results on top of operands, sizes whose
 kernels take several passes, other streams.  Tolerances are those of the arithmetic, as in the tests of the definitions."""
 import math
+import threading
 
 import pytest
 import torch
 
+import test_gpu_nn as base
 from paper_2306_16699_amd import rinr, rinr_nn as nn
 
 pytestmark = pytest.mark.gpu
@@ -355,3 +357,76 @@ def test_more_threads_than_a_launch_counts_along_x():
     assert bool((x[-1] == 5).all()) and bool((x[0] == -3).all()) and not x[1:1000].any() and not x[-1000:-1].any()
     del codes, scales, x
     torch.cuda.empty_cache()
+
+
+# ---- paths that take several passes ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(2100, 1500), (1100, 8200), (4200, 600), (3000, 4096)])
+def test_norms_whose_workgroups_take_several_rows(rows, cols, dtype):
+    """More rows than workgroups, a whole workgroup a row: scratch for the row's sums is used again, the gain's gradient adds up over rows."""
+    base.test_norm_is_its_definition(rows, cols, dtype)
+    base.test_norm_backward_is_its_definition(rows, cols, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 8200, 48), (16, 20000, 33), (64, 16384, 257), (3, 8191, 1), (40, 33000, 130)])
+def test_few_rows_whose_sum_several_workgroups_share(rows, n_in, n_out, dtype):
+    base.test_linear_is_its_definition(rows, n_in, n_out, dtype)
+    base.test_linear_backward_is_its_definition(rows, n_in, n_out, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(1, 33), (1100, 100), (2100, 1500), (5, 8200)])
+def test_norms_in_place(rows, cols, dtype):
+    """h may be x or the residual, dh may be dy or dres: the C entry is called so, and its results are those of separate memory."""
+    dt, L = DTYPES[dtype], nn.lib()
+    t = nn.TYPES[dt]
+    g = gen(rows + cols)
+    x, r, dy, dres = (torch.randn(rows, cols, generator=g, device="cuda").to(dt) for _ in range(4))
+    gain = torch.rand(cols, generator=g, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    y, h = nn.rms_norm(x, gain, residual=r)
+    for k in range(2):
+        both, got = [x.clone(), r.clone()], torch.empty_like(x)
+        a = nn._NORM.pack(rows, cols, both[0].data_ptr(), cols, both[1].data_ptr(), cols, gain.data_ptr(), got.data_ptr(), cols, 0, both[k].data_ptr(), cols, t, t, 1e-6, 0)
+        assert L.rinr_rms_norm(a, stream) == rinr.OK
+        assert torch.equal(got, y) and torch.equal(both[k], h) and torch.equal(both[1 - k], (x, r)[1 - k])
+    dh, dgain = nn.rms_norm_backward(dy, h, gain, dres=dres)
+    need = L.rinr_rms_norm_backward_workspace_bytes(rows, cols)
+    work = torch.empty(need, device="cuda", dtype=torch.uint8)
+    for k in range(2):
+        both, got = [dy.clone(), dres.clone()], torch.empty_like(gain)
+        a = nn._NORM_GRAD.pack(rows, cols, both[0].data_ptr(), cols, h.data_ptr(), cols, gain.data_ptr(), both[1].data_ptr(), cols, both[k].data_ptr(), cols, got.data_ptr(), t, 1e-6)
+        assert L.rinr_rms_norm_backward(a, work.data_ptr(), need, stream) == rinr.OK
+        assert torch.equal(got, dgain) and torch.equal(both[k], dh) and torch.equal(both[1 - k], (dy, dres)[1 - k])
+
+
+def test_calls_from_several_threads():
+    """Four threads, a stream each, the same operators at sizes of their own: results are those of one thread."""
+    jobs = []
+    for k in range(4):
+        g = gen(20 + k)
+        rows, n_in, n_out = 70 + 300 * k, 256 + 32 * k, 512
+        jobs.append((torch.randn(rows, n_in, generator=g, device="cuda").to(torch.bfloat16), torch.ones(n_in, device="cuda"),
+                     torch.randn(n_out, n_in, generator=g, device="cuda").to(torch.bfloat16), torch.zeros(n_out, device="cuda"),
+                     torch.randn(n_in, n_out, generator=g, device="cuda").to(torch.bfloat16), torch.zeros(n_in, device="cuda"),
+                     torch.randn(rows, n_in, generator=g, device="cuda").to(torch.bfloat16)))
+    want = [base.training_step(*j) for j in jobs]
+    torch.cuda.synchronize()
+    got = [None] * 4
+
+    def work(k):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            got[k] = [base.training_step(*jobs[k]) for _ in range(20)]
+        stream.synchronize()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for k in range(4):
+        for one in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(one, want[k])), k

@@ -318,10 +318,11 @@ template <class T, int NI, int NJ, int AT_ONCE> __device__ __forceinline__ void 
 // ---- operands on their way to LDS ------------------------------------------------------------------------------------------------------
 
 // 16 bytes a lane from base + at straight to LDS, a wavefront's 1024 bytes in a row.  Written as one block so that the compiler, which cannot tell
-// the LDS buffers apart, does not wait for it before it reads another one: barrier_with does.
+// the LDS buffers apart, does not wait for it before it reads another one: barrier_with does.  What it writes, m0 and LDS, is named: nothing is kept in m0 and no access of
+// LDS is moved across it.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void direct_16(const i32x4 base, uint32_t at, uint32_t lds_at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_at), "v"(at), "s"(base));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_at), "v"(at), "s"(base) : "m0", "memory");
 }
 // A barrier behind all but the last N of this wavefront's loads and all of its LDS accesses
 template <int N> __device__ __forceinline__ void barrier_with() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }

@@ -122,12 +122,16 @@ def main():
     store, labels = colour_store(a.images, a.classes)
     net = Backbone(a.patch, a.width, a.hidden, a.blocks, a.classes)
     g = torch.Generator().manual_seed(1)
-    t = time.perf_counter()
+    t = 0.0
     for step in range(a.steps):
         ids = torch.randint(0, a.images, (a.batch,), generator=g).to("cuda:0")
         loss = net.step(store.decode_batch(ids, a.size, a.size), labels[ids], a.lr)
         if step % 10 == 0 or step == a.steps - 1:
-            print(f"step {step}: cross entropy {loss.item():.4f}, {(time.perf_counter() - t) * 1e3 / (step + 1):.2f} ms a step", flush=True)
+            value = loss.item()
+            if step == 0:                                              # without what the first step sets up
+                t = time.perf_counter()
+            took = f", {(time.perf_counter() - t) * 1e3 / step:.2f} ms a step" if step else ""
+            print(f"step {step}: cross entropy {value:.4f}{took}", flush=True)
 
 
 if __name__ == "__main__":

@@ -23,8 +23,8 @@
  * beyond 65504, has the gradient that the finite one has, but for the sine.
  *
  * Sums (products, norms, gradients of bias and gain) are held in 32 bits.  Products of 32-bit operands take each operand as three
- * bf16 parts that add up to it and leave out what is below 2^-22 of a product; an infinity in such an operand makes results
- * NaN where 32-bit arithmetic would keep the infinity.  Results are the same bits from call to call on one GPU.
+ * bf16 parts that add up to it and leave out what is below 2^-21 of a product; parts are cut off, so that has the product's sign.  An infinity in such an
+ * operand makes results NaN where 32-bit arithmetic would keep the infinity.  Results are the same bits from call to call on one GPU.
  */
 #ifndef RINR_NN_H
 #define RINR_NN_H

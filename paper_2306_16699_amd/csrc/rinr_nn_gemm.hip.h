@@ -415,7 +415,8 @@ template <class E, int MODE, bool K_ROWS, int WIDE, int BK, int THREADS> struct 
 
 // Each operand as three bf16 parts.  4 wavefronts of 64 x 64, k staged through registers into one LDS buffer, so that two workgroups share a CU: what the
 // next k tile needs is under way while this one's matrix steps run.  (Two buffers, one workgroup a CU and the split between the matrix steps: 50176 x
-// 256 x 256 in 94 us, not 59.)  Bound by the two phases taking turns: 784 tiles there, matrix steps alone would take 16 us, the split 10.
+// 256 x 256 in 94 us, not 59.)  That product takes 55 us, with a sine: 784 tiles on 512 places are 1.53 rounds that cost two, and by its counters matrix pipes are 35 % busy,
+// vector instructions (split, addresses, sine) 44 %, LDS 10 %: the two workgroups of a CU overlap little of these phases.
 template <bool KP, bool KQ> __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_kernel(const GemmArgs a) {
     typedef bf16 E;
     constexpr int BK = kTileK, PARTS = 3, PLANE = kTile * BK, SIDE = PLANE * PARTS;
@@ -504,7 +505,8 @@ template <int WIDE_P_, int WIDE_Q_, int NI_, int NJ_> struct WideShape {
 // instructions: memory and LDS take an instruction of a wavefront only so often, and what waits for them holds up what is behind it.
 // 256 x 256 tiles are what L2 and LDS bandwidth allow (each value from LDS is used by 64 or 128 others, each from L2 by 256); 8 wavefronts, two a SIMD,
 // hide each other's waits.  Bound by the matrix pipe in the loop (66 % busy at 4096 values of k, at the card's power limit) and by what a tile's start and
-// results take, 11 us that nothing overlaps: 32768 rows in bf16, 4096 -> 4096 793 us (1386 TFLOP/s), 1024 -> 4096 303 (907), with GELU and z in 8 bits 347.
+// results take, 9 to 11 us that nothing overlaps: 32768 rows in bf16, 4096 -> 4096 784 us (1403 TFLOP/s, 1.39 us a k tile), 1024 -> 4096 248 (1108), with GELU 299, and z
+// in 8 bits 329.
 template <class E, class S, int MP, bool KP, int MQ, bool KQ> __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void wide_kernel(const GemmArgs a) {
     constexpr int BK = S::BK, NI = S::NI, NJ = S::NJ;
     static_assert(NI >= NJ, "");
@@ -629,7 +631,7 @@ template <class E, class S, int MP, bool KP, int MQ, bool KQ> __global__ __launc
 // 16 NJ rows of the result against 16 columns a workgroup, both operands with k side by side and straight from memory to the matrix steps: the
 // weights are read once (by each 16 NJ rows), by the whole GPU at once, and that is what the time goes to.  8 wavefronts share k in blocks of 64 (a lane
 // has 16 neighbouring values of it, so that 4 lanes read 128 bytes of a row) and add up through LDS.  Bound by a launch and two latencies (1 x 1024 ->
-// 4096 in bf16 4.7 us, 64 x 1024 -> 1000 5.1), for large weights by memory: 16 x 4096 -> 4096 11.1 us, 3.0 TB/s.
+// 4096 in bf16 4.4 us, 64 x 1024 -> 1000 5.1), for large weights by memory: 16 x 4096 -> 4096 10.8 us, 3.1 TB/s.
 constexpr int kFewWaves = 8, kFewBlock = 64, kFewColumns = 16;
 template <class T, class E, int PARTS, int SP, int SQ, int NJ> __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const GemmArgs a) {
     constexpr int AHEAD = NJ * PARTS <= 3 ? 4 : NJ * PARTS <= 6 ? 2 : 1, LD = 20;                              // blocks whose loads are under way together; a row of sums in LDS

@@ -49,7 +49,7 @@ struct NormArgs {
 
 // y = gain h / sqrt(mean h^2 + eps), h = x + residual.  A row stays in registers from the one time it is read; TPR threads share it and
 // each holds NV groups of 8 neighbouring columns: a wavefront up to 1024 columns, so that the sum needs no barrier.  Bound by memory: 32768 x 1024 in bf16
-// with residual 41 us (6.5 TB/s), with 8-bit output 36.
+// with residual 40 us (6.7 TB/s, part of it from the cache; 131072 rows 5.9), with 8-bit output 36.
 template <class T, int TPR, int NV, bool PACKED> __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormArgs a) {
     constexpr int THREADS = TPR < 256 ? 256 : TPR, SLOTS = THREADS / TPR;
     __shared__ float scratch[2 * THREADS / 64];
@@ -98,7 +98,7 @@ struct NormGradArgs {
 };
 
 // dh = s (g - u mean(g u)) + dres with u = h s, g = dy gain.  A workgroup takes every gridDim.x-th group of rows and keeps its columns' sums of
-// dy u in registers until the end.  Bound by memory: 32768 x 1024 in bf16 with the residual's gradient 45 us (6.0 TB/s), and 4.7 for the sums of 1024 workgroups.
+// dy u in registers until the end.  Bound by memory: 32768 x 1024 in bf16 with the residual's gradient 44 us (6.1 TB/s), and 4.7 for the sums of 1024 workgroups.
 template <class T, int TPR, int NV> __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(const NormGradArgs a) {
     constexpr int THREADS = TPR < 256 ? 256 : TPR, SLOTS = THREADS / TPR;
     __shared__ float scratch[2 * THREADS / 64];
@@ -189,8 +189,8 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(const float *part, int6
 
 // ---- 8-bit checkpoints ----------------------------------------------------------------------------------------------------------------
 
-// Four lanes take a block of 32 columns, 8 each; groups of 8 columns are numbered row by row over whole blocks.  Bound by memory: 134 M values of bf16 72 us
-// (5.6 TB/s), back 59 (6.8), back through GELU 84 (its 17 vector instructions a value).
+// Four lanes take a block of 32 columns, 8 each; groups of 8 columns are numbered row by row over whole blocks.  Bound by memory: 134 M values of bf16 71 us
+// (5.7 TB/s), back 58 (7.0), back through GELU 90 (its 19 vector instructions a value).
 template <class T> __global__ __launch_bounds__(256) void pack_kernel(int64_t rows, int cols, const T *x, int64_t ld_x, int8_t *codes, int64_t ld, uint8_t *scales, bool past) {
     const int64_t per_row = (cols + kBlock8 - 1) / kBlock8 * 4;
     const int64_t at = block_of() * 256 + threadIdx.x;
